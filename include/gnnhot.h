@@ -538,6 +538,8 @@ int32_t gnn_gather_rows(const void *src, int64_t ld_src, int32_t n_src, const in
  *   master      nullable; with bfloat16 parameters: their float copy, which is updated and rounded into param.
  *               Without it the update is computed in float from the bfloat16 value and rounded to nearest: updates
  *               below half a step of bfloat16 (2^-9 of the weight) are lost.
+ * eps         at least 1e-16: below that, second moments in float (8-bit blocks end at 2^-126) are too coarse to divide by alone, and the step of a
+ *               weight with tiny gradients would be m / eps in place of the formula's.
  * Tensors must not overlap.
  */
 typedef struct gnn_param {
@@ -566,7 +568,7 @@ typedef struct gnn_step_state {
 } gnn_step_state;
 
 typedef struct gnn_adamw_hyper {
-    double lr, beta1, beta2, eps;  /* lr >= 0, 0 <= beta < 1, eps > 0 */
+    double lr, beta1, beta2, eps;  /* lr >= 0, 0 <= beta < 1, 1e-16 <= eps <= 1e30 */
     int64_t step;                  /* number of this step, from 1; read without a gnn_step_state only */
     float grad_scale;              /* factor of the gradients; read without a gnn_step_state only */
 } gnn_adamw_hyper;

@@ -179,6 +179,12 @@ struct AdamArgs {
     double lr, beta1, beta2;
 };
 
+// eps is what divides the update where a second moment in float is too small to: the square of a gradient below 2^-75 is no float, and a
+// block of 8-bit moments ends at 2^-126, whose root, corrected for beta2 = 0.999's first step, is 3.4e-18.  With an eps below that the step of
+// such a weight would be m / eps, larger without bound than the formula's; below 2.9e-39 even 1 / eps is infinite, and a weight
+// that nothing has reached (m = 0) would become NaN.  The upper end keeps the reciprocal a normal float.
+constexpr float kEpsLeast = 1e-16f, kEpsMost = 1e30f;
+
 // beta^t by squaring; t is the same for every lane
 __device__ __forceinline__ double power(double b, int64_t t) {
     double r = 1.0;
@@ -461,7 +467,8 @@ extern "C" int32_t gnn_adamw_step(const gnn_param* params, int32_t n_params, int
     GNN_REQUIRE(hyper != nullptr, GNN_ERR_INVALID_ARG, "hyper is NULL");
     GNN_REQUIRE(hyper->beta1 >= 0.0 && hyper->beta1 < 1.0 && hyper->beta2 >= 0.0 && hyper->beta2 < 1.0, GNN_ERR_INVALID_ARG,
                 "beta1 = %g, beta2 = %g: out of [0, 1)", hyper->beta1, hyper->beta2);
-    GNN_REQUIRE((float)hyper->eps > 0.f && isfinite((float)hyper->eps), GNN_ERR_INVALID_ARG, "eps = %g is not a positive float", hyper->eps);
+    GNN_REQUIRE((float)hyper->eps >= kEpsLeast && (float)hyper->eps <= kEpsMost, GNN_ERR_INVALID_ARG, "eps = %g is out of [%g, %g]", hyper->eps,
+                (double)kEpsLeast, (double)kEpsMost);
     GNN_REQUIRE(isfinite(hyper->lr) && hyper->lr >= 0.0, GNN_ERR_INVALID_ARG, "lr = %g", hyper->lr);
     GNN_REQUIRE(state != nullptr || hyper->step >= 1, GNN_ERR_INVALID_ARG, "step = %lld: the first step is 1", (long long)hyper->step);
     GNN_REQUIRE(state != nullptr || isfinite(hyper->grad_scale), GNN_ERR_INVALID_ARG, "grad_scale is not finite");

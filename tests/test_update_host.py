@@ -80,6 +80,16 @@ def test_adamw_refuses(lib, bad):
     assert lib.gnn_adamw_step(P256, 1, 1, C.byref(h), None, None, None) == 1
 
 
+@pytest.mark.parametrize("eps,status", [(1e-40, 1), (1.1e-38, 1), (1e-30, 1), (1e-18, 1), (9.9e-17, 1), (1.1e30, 1), (-1e-8, 1), (math.nan, 1),
+                                        (1e-16, 0), (1e-15, 0), (1e-8, 0), (1.0, 0), (1e30, 0)])
+def test_adamw_takes_an_eps_that_floats_can_divide_by(lib, eps, status):
+    """Below 2.9e-39 the reciprocal of eps is infinite and a weight with zero moments became NaN; below the root of the smallest second
+    moment that is kept the step of a weight with tiny gradients was m / eps.  No tensors: an accepted call does nothing."""
+    h = B.gnn_adamw_hyper(lr=1e-3, beta1=0.9, beta2=0.999, eps=eps, step=1, grad_scale=1.0)
+    assert lib.gnn_adamw_step(None, 0, 0, C.byref(h), None, None, None) == status
+    assert status == 0 or b"eps" in lib.gnn_last_error()
+
+
 def test_adamw_refuses_tables(lib):
     h = B.gnn_adamw_hyper(1e-3, 0.9, 0.999, 1e-8, 1, 1.0)
     assert lib.gnn_adamw_step(P256, 1, 1, None, None, None, None) == 1
