@@ -230,6 +230,24 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
     return top < 0x00800000u ? 0.f : __uint_as_float(top);
 }
 
+// Root of the instruction set, good to an ulp.  It takes a subnormal for zero: a lane that has one (a pattern of 1 .. 2^23 - 1) takes its
+// four roots again, 2^64 times as large, so that 2^-126 and the values below it divide as the formula says.  Ordinary
+// values pay for the question alone.
+__device__ __forceinline__ void roots(const float (&v)[4], float (&r)[4]) {
+    uint32_t least = 0xffffffffu;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t b = __float_as_uint(v[e]) - 1u;      // of zero: the largest
+        least = b < least ? b : least;
+        r[e] = __builtin_amdgcn_sqrtf(v[e]);
+    }
+    if (least < 0x007fffffu) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (__float_as_uint(v[e]) < 0x00800000u) r[e] = __builtin_amdgcn_sqrtf(v[e] * 0x1p64f) * 0x1p-32f;
+    }
+}
+
 // A wavefront takes 256 elements at a time, four a lane: 16-byte loads and stores of floats, and exactly one block of an 8-bit state, whose
 // largest value is then a reduction inside the wavefront.  Bound: HBM.  28 bytes an element with float states, 16 with 8-bit states:
 // 247M elements in 8 bits 840 us (4.7 TB/s; a copy of 4 GB runs at 4.8), 59M 190 to 218 us, 0.46M with float states 5.5 us.
@@ -274,8 +292,12 @@ __device__ __forceinline__ void adamw_four(const AdamTensor& t, int64_t i, const
         const float gs = g[e] * coef;
         m[e] = m[e] * a.b1 + gs * a.ob1;
         v[e] = v[e] * a.b2 + (gs * gs) * a.ob2;
-        // root and reciprocal of the instruction set, an ulp each (a v below 2^-126 has the root 0)
-        const float den = __builtin_amdgcn_sqrtf(v[e]) * inv_root + a.eps;
+    }
+    float root[4];
+    roots(v, root);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float den = root[e] * inv_root + a.eps;      // at least kEpsLeast
         p[e] = p[e] * t.decay - (m[e] * __builtin_amdgcn_rcpf(den)) * step_size;
         if (BITS == 8 && (VEC || i + e < n)) {
             const uint32_t x = __float_as_uint(m[e]) & 0x7fffffffu, y = __float_as_uint(v[e]) & 0x7fffffffu;

@@ -168,6 +168,30 @@ def test_more_chunks_than_workgroups():
     run([one(rng, 9_000_001, bits=8), one(rng, 300), one(rng, 700_000, "master")], 1.0)
 
 
+@pytest.mark.parametrize("step", [1, 100, 10 ** 6])
+def test_second_moments_below_the_normal_floats_divide(step):
+    """Their root counts where eps is small: at eps = 1e-16 and the first steps 1 % of what divides.  The gradients are zero, so the new
+    second moment is one product, in subnormals half a step of 2^-149 off; weights are zero, so that the update is what is compared."""
+    rng = np.random.default_rng(21)
+    n = 1000
+    h, e = one(rng, n)
+    h["p"][:], h["g"][:] = 0, 0
+    h["v"] = (2.0 ** -rng.uniform(126.5, 140, n)).astype(f32)
+    h["v"][::7] = f32(1e-6)       # ordinary ones and zeros beside them
+    h["v"][::11] = 0
+    h["m"] = (rng.standard_normal(n) * 1e-17).astype(f32)
+    for key, name in (("p", "param"), ("g", "grad"), ("m", "m"), ("v", "v")):
+        e[name].copy_(torch.from_numpy(h[key]))
+    eps = float(f32(1e-16))
+    P.gnn_adamw_step(P.ParamTable([e]), 1e-3, HYP["betas"], eps, step=step)
+    v = h["v"] * f32(0.999)       # what the state holds
+    assert np.array_equal(e["v"].cpu().numpy(), v) and (v < 2.0 ** -126).sum() > n // 2
+    upd = 1e-3 / (1 - 0.9 ** step) * 0.9 * h["m"].astype(np.float64) / (np.sqrt(v.astype(np.float64) / (1 - 0.999 ** step)) + eps)
+    got = -e["param"].double().cpu().numpy()
+    # coefficient of m, m, factor of the step, root and its factor (2 u for an ulp), their product, the sum, reciprocal, two products: 12 u
+    assert (np.abs(got - upd) <= 12 * U * np.abs(upd)).all(), np.max(np.abs(got - upd) / np.maximum(np.abs(upd), 1e-60)) / U
+
+
 @pytest.mark.parametrize("step", [1, 2, 1000, 10 ** 7])
 def test_step_numbers(step):
     run([one(np.random.default_rng(1), 1000)], step=step)
