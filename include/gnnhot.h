@@ -584,7 +584,7 @@ int32_t gnn_param_layout(gnn_param *params_host, int32_t n_params, int64_t *n_ch
  * Norm of all gradients, the factor that clips them, and the number of the step, to *state (device): two launches.
  *   grad_scale  factor of every gradient (1 / the number of micro-batches they were added up over, say); finite
  *   max_norm    0 or less: no clipping
- * The sum is formed in 64 bits in a fixed order.  If it is not finite the step is refused: state->ok = 0, skipped + 1, step
+ * The sum is formed in 64 bits in a fixed order.  If the norm is not finite as a float the step is refused: state->ok = 0, skipped + 1, step
  * stays, and gnn_adamw_step with this state changes nothing.  Workspace: (ws, ws_bytes) size-query protocol.
  */
 int32_t gnn_grad_norm(const gnn_param *params, int32_t n_params, int64_t n_chunks, float grad_scale, float max_norm,

@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256) void norm_state_kernel(const double* __restric
     total = block_sum(total, lds);
     if (threadIdx.x != 0) return;
     const double norm = fabs((double)grad_scale) * sqrt(total);
-    const bool ok = isfinite(norm);
+    const bool ok = isfinite((float)norm);     // as it is stored: finite gradients whose norm is no float are refused too
     state->ok = ok;
     state->sum_sq = total;
     state->norm = (float)norm;

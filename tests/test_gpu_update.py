@@ -224,6 +224,24 @@ def test_a_step_with_an_infinite_gradient_changes_nothing(poison):
     assert (opt.state.ok.item(), opt.state.step.item(), opt.state.skipped.item()) == (1, 5, 1)
 
 
+@pytest.mark.parametrize("grad_scale,refused", [(1.0, True), (-1.0, True), (0.25, False), (1e-3, False)])
+def test_a_norm_that_is_no_float_refuses_the_step(grad_scale, refused):
+    """Four gradients of 3e38 are finite, their norm of 6e38 is not a float: what is stored as infinite is not taken."""
+    h, e = one(np.random.default_rng(22), 4)
+    h["g"][:] = 3e38
+    e["grad"].fill_(3e38)
+    before = {k: e[k].clone() for k in ("param", "m", "v")}
+    table, state = P.ParamTable([e]), P.StepState(6)
+    P.gnn_grad_norm(table, state, grad_scale, 1.0)
+    P.gnn_adamw_step(table, HYP["lr"], HYP["betas"], HYP["eps"], state=state)
+    assert math.isinf(state.norm.item()) == refused and state.ok.item() == (0 if refused else 1)
+    assert (state.step.item(), state.skipped.item()) == ((6, 1) if refused else (7, 0))
+    for k, t in before.items():
+        assert torch.equal(e[k], t) == refused, k
+    if not refused:
+        check_update(h, e, state.coef.item(), 7)
+
+
 def test_8_bit_blocks_of_zeros_tiny_values_and_nan():
     h, e = one(np.random.default_rng(8), 1024 + 7, bits=8)
     for key in ("m", "v"):
