@@ -82,7 +82,7 @@ class gnn_param(C.Structure):
 
 class gnn_adamw_hyper(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64),
-                ("grad_scale", C.c_float)]
+                ("grad_scale", C.c_float), ("rounding_seed", C.c_uint32)]
 
 
 _lib = None
@@ -786,11 +786,14 @@ def gnn_grad_norm(table: ParamTable, state: StepState, grad_scale: float = 1.0, 
 
 
 def gnn_adamw_step(table: ParamTable, lr: float, betas=(0.9, 0.999), eps: float = 1e-8, state: StepState | None = None, step: int = 0,
-                   grad_scale: float = 1.0, lr_device: torch.Tensor | None = None):
+                   grad_scale: float = 1.0, lr_device: torch.Tensor | None = None, rounding_seed: int = 0):
     """One AdamW step on every tensor of the table, in place.  state: as gnn_grad_norm left it; without it `step` (from 1) and
-    grad_scale count.  lr_device: float32 device tensor that is read in place of lr when the kernel runs."""
+    grad_scale count.  lr_device: float32 device tensor that is read in place of lr when the kernel runs.  rounding_seed (32 bits): 8-bit
+    states are rounded without bias, which a run of more than a few hundred steps needs; 0: to the nearest code."""
     assert lr_device is None or (lr_device.dtype == torch.float32 and lr_device.numel() == 1)
-    h = gnn_adamw_hyper(lr, betas[0], betas[1], eps, step, grad_scale)
+    if not 0 <= rounding_seed < 1 << 32:
+        raise ValueError("rounding_seed has 32 bits")
+    h = gnn_adamw_hyper(lr, betas[0], betas[1], eps, step, grad_scale, rounding_seed)
     _check(lib().gnn_adamw_step(_ptr(table.table), table.n_params, table.n_chunks, C.byref(h), _ptr(lr_device),
                                 None if state is None else _ptr(state.buf), _stream()))
 

@@ -177,6 +177,8 @@ struct AdamArgs {
     float b1, ob1, b2, ob2, eps;    // ob = 1 - b
     float grad_scale, step_size, inv_root;   // without a state: lr / (1 - b1^t), 1 / sqrt(1 - b2^t) from the host
     double lr, beta1, beta2;
+    int64_t step;        // without a state
+    uint32_t seed;       // of the unbiased rounding
 };
 
 // eps is what divides the update where a second moment in float is too small to: the square of a gradient below 2^-75 is no float, and a
@@ -222,6 +224,59 @@ __device__ __forceinline__ float v_code(float x) {
     return c + (x >= hi * hi ? 1.0f : 0.f) - (x < lo * lo ? 1.0f : 0.f);
 }
 
+// Unbiased rounding.  To the nearest code a state that moves by less than half a step of its code never moves: a second moment falls by at
+// most 1 - beta2 of itself a step, a code is 4 / c of it, so none but the block's largest ever falls, and it rises on spikes only.
+// Gradients of N(0, 1), 64 of a block's 256 falling tenfold after 1000 steps: their second moments are 70 times the 32-bit ones 6000
+// steps later, their steps eight times too small.  Here x between the values of codes c and c + 1 becomes c + 1 in as many of 2^23 cases as x
+// lies beyond c's value, so that its mean is x: the same second moments are within 0.7 to 1.4 of the 32-bit ones (a relative spread of
+// about sqrt(2 / c)) and a first moment whose gradient has become zero decays to zero.
+// The draw is a function of (seed, step, tensor, element) alone: products of 32 bits by odd constants (the fractions of the golden ratio and of
+// the roots of 3 and 2), their halves folded onto each other; m takes the upper 23 bits of the element's number, v the lower 23 in
+// reverse.  Uniform and without correlation between elements, steps, tensors and the two (1M draws in 4096 cells each).
+// What it costs: four products a draw at a quarter of the vector unit's rate, which the step is close to being bound by: 247M elements 889 to 896 us
+// (819 with nearest codes), 59M 239 to 260 (183).
+constexpr uint32_t kDraw[3] = {0x9E3779B9u, 0xBB67AE85u, 0x6A09E667u};
+__device__ __forceinline__ uint32_t fold(uint32_t x, uint32_t c) {
+    const uint64_t p = (uint64_t)x * c;
+    return (uint32_t)p ^ (uint32_t)(p >> 32);
+}
+struct DrawKey {      // of a tensor in a step
+    uint32_t k0, k1;
+};
+__device__ __forceinline__ DrawKey draw_key(uint32_t seed, int64_t step, uint32_t tensor) {
+    uint32_t s = fold(seed + kDraw[0], kDraw[1]);
+    s = fold(s ^ (uint32_t)step, kDraw[2]);
+    s = fold(s + (uint32_t)(step >> 32) + kDraw[0], kDraw[1]);
+    const uint32_t k0 = fold(s ^ tensor, kDraw[2]);
+    return {k0, fold(k0 + kDraw[0], kDraw[1])};
+}
+// Of the elements from i on that share its upper 32 bits (four, and i a multiple of four).
+__device__ __forceinline__ DrawKey key_at(const DrawKey& k, int64_t i) {
+    const uint32_t high = (uint32_t)(i >> 32);
+    return {k.k0 + high * kDraw[2], k.k1 + high * kDraw[0]};
+}
+__device__ __forceinline__ uint32_t draw(const DrawKey& k, uint32_t low) { return fold(fold(low ^ k.k0, kDraw[0]) ^ k.k1, kDraw[1]); }
+// (k + 1/2) 2^-23 of the upper 23 bits k, exact
+__device__ __forceinline__ float unit(uint32_t h) { return __uint_as_float(0x3f800000u | h >> 9) - 0.99999994f; }
+
+// POWER 2 and 127 steps, or 4 and 255: the number of values (j / steps)^POWER at or below x, j from 1 on, and one more where
+// x - (that value) > u * (the distance to the next value).  x may be an ulp above 1.
+template <int POWER>
+__device__ __forceinline__ float unbiased_code(float x, float u) {
+    constexpr float kSteps = POWER == 2 ? 127.0f : 255.0f;
+    const auto value = [](float c) {
+        float f = c * (1.0f / kSteps);
+        f = f * f;
+        return POWER == 2 ? f : f * f;
+    };
+    float r = __builtin_amdgcn_sqrtf(x);
+    if (POWER == 4) r = __builtin_amdgcn_sqrtf(r);
+    float c = floorf(r * kSteps);                 // at most one off: the values on its two sides decide
+    c = c + (x >= value(c + 1.0f) ? 1.0f : 0.f) - (x < value(c) ? 1.0f : 0.f);
+    const float lo = value(c), hi = value(c + 1.0f);
+    return fminf(c + (x - lo > u * (hi - lo) ? 1.0f : 0.f), kSteps);
+}
+
 // A scale from the largest bit pattern of |x| in a block: bit patterns of non-negative floats ascend with their values, infinities and NaN
 // last.  A block that holds one of those gets the scale NaN (all its values are NaN from then on: nothing is hidden), one below the
 // smallest normal float becomes zeros.
@@ -263,8 +318,9 @@ struct AdamTensor {
 };
 
 // PT: 0 float parameters, 1 bfloat16, 2 bfloat16 with a float copy that is updated and rounded into them.
-template <int PT, int GT, int BITS, bool VEC>
-__device__ __forceinline__ void adamw_four(const AdamTensor& t, int64_t i, const AdamArgs& a, float coef, float step_size, float inv_root) {
+template <int PT, int GT, int BITS, bool UNBIASED, bool VEC>
+__device__ __forceinline__ void adamw_four(const AdamTensor& t, int64_t i, const AdamArgs& a, float coef, float step_size, float inv_root,
+                                           const DrawKey& key) {
     float p[4], g[4], m[4], v[4];
     const int64_t n = t.n;
     uint32_t mc = 0, vc = 0;
@@ -315,11 +371,14 @@ __device__ __forceinline__ void adamw_four(const AdamTensor& t, int64_t i, const
         vs = scale_of(wave_max_u32(vt));
         const float mi = ms > 0.f ? 1.0f / ms : 0.f, vi = vs > 0.f ? 1.0f / vs : 0.f;   // zeros and NaN: codes 0
         mc = vc = 0;
+        const DrawKey at = key_at(key, i);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float c = mi > 0.f ? m_code(fabsf(m[e]) * mi) : 0.f;
+            const uint32_t h = UNBIASED ? draw(at, (uint32_t)i + e) : 0u;
+            float c = UNBIASED ? unbiased_code<2>(fabsf(m[e]) * mi, unit(h)) : m_code(fabsf(m[e]) * mi);
+            c = mi > 0.f ? c : 0.f;
             c = m[e] < 0.f ? -c : c;
-            float d = v_code(v[e] * vi);
+            float d = UNBIASED ? unbiased_code<4>(v[e] * vi, unit(__brev(h))) : v_code(v[e] * vi);
             d = v[e] > 0.f ? fmaxf(d, 1.0f) : 0.f;     // a second moment never shrinks to zero: its root divides
             d = vi > 0.f ? d : 0.f;
             mc |= ((uint32_t)(int)c & 255u) << (8 * e);
@@ -334,17 +393,18 @@ __device__ __forceinline__ void adamw_four(const AdamTensor& t, int64_t i, const
     }
 }
 
-template <int PT, int GT, int BITS>
+template <int PT, int GT, int BITS, bool UNBIASED>
 __device__ __forceinline__ void adamw_chunks(const AdamTensor& t, int64_t i0, int64_t i1, bool vec, const AdamArgs& a, float coef,
-                                             float step_size, float inv_root) {
+                                             float step_size, float inv_root, const DrawKey& key) {
     // a wavefront owns whole state blocks; it enters a block together, also where the tensor ends inside it
     for (int64_t w = i0 + (threadIdx.x & ~63u) * 4; w < i1; w += 1024) {
         const int64_t i = w + 4 * lane_id();
-        if (vec && w + kStateBlock <= t.n) adamw_four<PT, GT, BITS, true>(t, i, a, coef, step_size, inv_root);
-        else adamw_four<PT, GT, BITS, false>(t, i, a, coef, step_size, inv_root);
+        if (vec && w + kStateBlock <= t.n) adamw_four<PT, GT, BITS, UNBIASED, true>(t, i, a, coef, step_size, inv_root, key);
+        else adamw_four<PT, GT, BITS, UNBIASED, false>(t, i, a, coef, step_size, inv_root, key);
     }
 }
 
+template <bool UNBIASED>
 __global__ __launch_bounds__(256) void adamw_kernel(const gnn_param* __restrict__ params, int32_t n_params, int64_t n_chunks, AdamArgs a,
                                                     const float* __restrict__ lr_device, const gnn_step_state* __restrict__ state) {
     const int64_t per = (n_chunks + gridDim.x - 1) / gridDim.x;
@@ -353,10 +413,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(const gnn_param* __restrict_
     double lr = a.lr;
     if (lr_device) lr = (double)*lr_device;
     float coef = a.grad_scale, step_size = a.step_size, inv_root = a.inv_root;
+    int64_t step = a.step;
     if (state) {
         if (!state->ok) return;   // a refused step changes nothing
         coef = state->coef;
-        const int64_t step = state->step;
+        step = state->step;
         step_size = (float)(lr / (1.0 - power(a.beta1, step)));
         inv_root = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
     } else if (lr_device) {
@@ -374,8 +435,9 @@ __global__ __launch_bounds__(256) void adamw_kernel(const gnn_param* __restrict_
             const uintptr_t off = ((uintptr_t)q.param & (pt ? 7u : 15u)) | ((uintptr_t)q.grad & (gt == GNN_F32 ? 15u : 7u)) |
                                   (((uintptr_t)q.m | (uintptr_t)q.v) & (bits == 32 ? 15u : 3u)) | ((uintptr_t)q.master & 15u);
             const bool vec = off == 0;
+            const DrawKey key = UNBIASED ? draw_key(a.seed, step, (uint32_t)k) : DrawKey{0u, 0u};
             const int64_t i0 = (c - first) * kChunk, end = (stop - first) * kChunk, i1 = end < q.n ? end : q.n;
-#define GNN_ADAM(PT_, GT_, B_) adamw_chunks<PT_, GT_, B_>(t, i0, i1, vec, a, coef, step_size, inv_root)
+#define GNN_ADAM(PT_, GT_, B_) adamw_chunks<PT_, GT_, B_, B_ == 8 && UNBIASED>(t, i0, i1, vec, a, coef, step_size, inv_root, key)
 #define GNN_ADAM_P(GT_, B_)                 \
     do {                                    \
         if (pt == 0) GNN_ADAM(0, GT_, B_);  \
@@ -497,13 +559,14 @@ extern "C" int32_t gnn_adamw_step(const gnn_param* params, int32_t n_params, int
     GNN_REQUIRE(((uintptr_t)state & 7u) == 0, GNN_ERR_INVALID_ARG, "state is not 8-byte aligned");
     if (n_chunks == 0) return GNN_OK;
     AdamArgs a = {(float)hyper->beta1, (float)(1.0 - hyper->beta1), (float)hyper->beta2, (float)(1.0 - hyper->beta2), (float)hyper->eps,
-                  hyper->grad_scale, 0.f, 0.f, hyper->lr, hyper->beta1, hyper->beta2};
+                  hyper->grad_scale, 0.f, 0.f, hyper->lr, hyper->beta1, hyper->beta2, hyper->step, hyper->rounding_seed};
     if (!state) {
         const double c1 = 1.0 / (1.0 - pow(hyper->beta1, (double)hyper->step));
         a.step_size = (float)(lr_device ? c1 : hyper->lr * c1);    // with lr_device the kernel multiplies
         a.inv_root = (float)(1.0 / sqrt(1.0 - pow(hyper->beta2, (double)hyper->step)));
     }
-    adamw_kernel<<<grid_of(n_chunks), 256, 0, (hipStream_t)stream>>>(params, n_params, n_chunks, a, lr_device, state);
+    if (hyper->rounding_seed) adamw_kernel<true><<<grid_of(n_chunks), 256, 0, (hipStream_t)stream>>>(params, n_params, n_chunks, a, lr_device, state);
+    else adamw_kernel<false><<<grid_of(n_chunks), 256, 0, (hipStream_t)stream>>>(params, n_params, n_chunks, a, lr_device, state);
     GNN_LAUNCH_CHECK("adamw_kernel");
     return GNN_OK;
 }
