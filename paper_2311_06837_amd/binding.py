@@ -862,9 +862,11 @@ def gnn_linear_i8_fwd(rows, n_active: int, A_neigh: torch.Tensor, scale_neigh, X
     N = W_neigh.N
     assert rows is None or rows.numel() >= n_active
     need = n_active if rows is None else 0
-    assert W_neigh.K == K and A_neigh.shape[1] >= ((K + 15) // 16 * 16 if codes else K) and H_out.shape[1] >= N and min(A_neigh.shape[0], H_out.shape[0]) >= need
+    width = (K + 15) // 16 * 16 if codes else K     # codes are read in sixteens
+    assert W_neigh.K == K and A_neigh.shape[1] >= width and H_out.shape[1] >= N and min(A_neigh.shape[0], H_out.shape[0]) >= need
     if X_self is not None:
-        assert _mat(X_self, "X_self").dtype == A_neigh.dtype and X_self.stride(0) == A_neigh.stride(0) and X_self.shape[0] >= need and X_self.shape[1] >= K
+        assert _mat(X_self, "X_self").dtype == A_neigh.dtype and X_self.stride(0) == A_neigh.stride(0) and X_self.shape[0] >= need
+        assert X_self.shape[1] >= width, f"X_self: rows of {width} columns expected"
         assert W_self is not None and (W_self.K, W_self.N) == (K, N)
     for s in (scale_neigh, scale_self):
         assert s is None or (s.dtype == torch.float32 and s.is_contiguous() and s.numel() >= need)

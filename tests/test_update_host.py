@@ -138,6 +138,16 @@ def test_linear_i8_refuses(lib):
     assert lib.gnn_linear_i8_fwd(*args, None, C.byref(need), None) == 0
 
 
+def test_product_refuses_codes_that_end_inside_a_group_of_sixteen():
+    """The kernels read codes in groups of 16 columns: a matrix of X_self that ends at K may end inside the last one."""
+    torch = pytest.importorskip("torch")
+    w = B.Int8Weight(torch.zeros(B.Int8Weight.bytes(20, 9), dtype=torch.int8), torch.zeros(9), 20, 9)
+    A, s, H = torch.zeros(3, 32, dtype=torch.int8), torch.zeros(3), torch.zeros(3, 9)
+    X = torch.zeros(2 * 32 + 20, dtype=torch.int8).as_strided((3, 20), (32, 1))
+    with pytest.raises(AssertionError, match="X_self"):
+        B.gnn_linear_i8_fwd(None, 3, A, s, X, s, 20, w, w, None, H, False)
+
+
 def test_table_refuses_tensors_it_cannot_read():
     torch = pytest.importorskip("torch")
     with pytest.raises(ValueError, match="grad"):
