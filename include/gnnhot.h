@@ -576,7 +576,7 @@ typedef struct gnn_step_state {
 } gnn_step_state;
 
 typedef struct gnn_adamw_hyper {
-    double lr, beta1, beta2, eps;  /* lr >= 0, 0 <= beta < 1, 1e-16 <= eps <= 1e30 */
+    double lr, beta1, beta2, eps;  /* lr >= 0 and lr / (1 - beta1) a float, 0 <= beta < 1, 1e-16 <= eps <= 1e30 */
     int64_t step;                  /* number of this step, from 1; read without a gnn_step_state only */
     float grad_scale;              /* factor of the gradients; read without a gnn_step_state only */
     uint32_t rounding_seed;        /* 0: 8-bit states are rounded to the nearest code; else without bias, see state_bits */

@@ -553,7 +553,8 @@ extern "C" int32_t gnn_adamw_step(const gnn_param* params, int32_t n_params, int
                 "beta1 = %g, beta2 = %g: out of [0, 1)", hyper->beta1, hyper->beta2);
     GNN_REQUIRE((float)hyper->eps >= kEpsLeast && (float)hyper->eps <= kEpsMost, GNN_ERR_INVALID_ARG, "eps = %g is out of [%g, %g]", hyper->eps,
                 (double)kEpsLeast, (double)kEpsMost);
-    GNN_REQUIRE(isfinite(hyper->lr) && hyper->lr >= 0.0, GNN_ERR_INVALID_ARG, "lr = %g", hyper->lr);
+    // the first step's factor: infinite, it would make a weight that nothing has reached NaN
+    GNN_REQUIRE(hyper->lr >= 0.0 && isfinite((float)(hyper->lr / (1.0 - hyper->beta1))), GNN_ERR_INVALID_ARG, "lr = %g: lr / (1 - beta1) is no float", hyper->lr);
     GNN_REQUIRE(state != nullptr || hyper->step >= 1, GNN_ERR_INVALID_ARG, "step = %lld: the first step is 1", (long long)hyper->step);
     GNN_REQUIRE(state != nullptr || isfinite(hyper->grad_scale), GNN_ERR_INVALID_ARG, "grad_scale is not finite");
     GNN_REQUIRE(((uintptr_t)state & 7u) == 0, GNN_ERR_INVALID_ARG, "state is not 8-byte aligned");

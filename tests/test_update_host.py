@@ -90,6 +90,14 @@ def test_adamw_takes_an_eps_that_floats_can_divide_by(lib, eps, status):
     assert status == 0 or b"eps" in lib.gnn_last_error()
 
 
+@pytest.mark.parametrize("lr,beta1,status", [(1e39, 0.0, 1), (1e38, 0.9, 1), (math.inf, 0.9, 1), (math.nan, 0.9, 1), (-1e-9, 0.9, 1), (1e37, 0.9, 0), (0.0, 0.9, 0)])
+def test_adamw_takes_a_rate_whose_first_step_is_a_float(lib, lr, beta1, status):
+    """An infinite lr / (1 - beta1) times the zero update of a weight that nothing has reached was NaN."""
+    h = B.gnn_adamw_hyper(lr=lr, beta1=beta1, beta2=0.999, eps=1e-8, step=1, grad_scale=1.0)
+    assert lib.gnn_adamw_step(None, 0, 0, C.byref(h), None, None, None) == status
+    assert status == 0 or b"lr" in lib.gnn_last_error()
+
+
 def test_adamw_refuses_tables(lib):
     h = B.gnn_adamw_hyper(1e-3, 0.9, 0.999, 1e-8, 1, 1.0)
     assert lib.gnn_adamw_step(P256, 1, 1, None, None, None, None) == 1
