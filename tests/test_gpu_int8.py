@@ -254,6 +254,44 @@ def test_a_rows_answer_does_not_depend_on_the_others():
         assert torch.equal(H, outs[-1][: H.shape[0]])
 
 
+@pytest.mark.parametrize("K,N,src,sizes", [
+    (1091, 300, 1, (1, 20, 40, 1000, 11_000, 25_000)),      # few rows, then tiles of 64, of 128 (256 tiles of them), of 256 (192)
+    (1091, 300, 2, (1, 20, 40, 1000, 11_000)),              # two sources: tiles of 64 and 128
+    (602, 50, 1, (1, 20, 40, 1000, 33_000, 50_000)),        # codes of narrow outputs take the tiles, floats the panels
+    (602, 50, 2, (1, 20, 40, 1000, 33_000)),
+])
+@pytest.mark.parametrize("kind", [F, H16])
+def test_a_rows_answer_is_the_same_in_every_kernel(kind, K, N, src, sizes):
+    """Equal to the bit, from rows and from codes, with the neighbour half, the vertex's own, bias and ReLU; listed rows of the largest
+    size too."""
+    print(f"every kernel: K={K} N={N} src={src} {kind}", flush=True)
+    M, Kq = sizes[-1], (K + 15) // 16 * 16
+    X = [torch.randn(M, Kq, device="cuda").to(kind) for _ in range(src)]
+    w = [P.gnn_quantize_weight(torch.randn(K, N, device="cuda")) for _ in range(src)] + [None]
+    bias = torch.randn(N, device="cuda")
+    Q = [torch.zeros(M, Kq, dtype=torch.int8, device="cuda") for _ in range(src)]
+    s = [torch.zeros(M, device="cuda") for _ in range(src)]
+    for k in range(src):
+        P.gnn_quantize_rows(None, M, X[k], K, Q[k], s[k])
+
+    def answer(rows, n, codes):
+        x, sc = (Q, s) if codes else (X, [None] * src)
+        H = torch.full((M, N), 7.0, device="cuda")
+        P.gnn_linear_i8_fwd(rows, n, x[0], sc[0], x[1] if src == 2 else None, sc[1] if src == 2 else None, K, w[0], w[1], bias, H, True)
+        return H
+    want = answer(None, M, True)
+    for codes in (True, False):
+        for n in sizes:
+            H = answer(None, n, codes)
+            assert torch.equal(H[:n], want[:n]) and (H[n:] == 7).all(), (codes, n)
+        n = M - M // 50      # a list that still fills the largest tiles
+        ids = torch.randperm(M, device="cuda")[:n].to(torch.int32)
+        H = answer(ids, n, codes)
+        there = torch.zeros(M, dtype=torch.bool, device="cuda")
+        there[ids.long()] = True
+        assert torch.equal(H[there], want[there]) and (H[~there] == 7).all(), codes
+
+
 def test_product_long_reduction():
     product(65, 65536, 40, 1, "i8", F, False, False)
     product(2, 20_000, 33, 2, H16, F, False, False)
