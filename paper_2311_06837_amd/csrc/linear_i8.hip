@@ -112,8 +112,8 @@ __device__ __forceinline__ void slice_barrier() {
 // Long reductions: WM x WN wavefronts, each MT x NT blocks of 32 x 32 of the output.  The reduction moves in slices of 64 bytes through a ring
 // of R LDS buffers that the loads fill themselves (no registers in between): R - 1 slices are on their way or being multiplied, one
 // barrier a slice.  With two buffers of 128 bytes every slice waited for loads that had been asked for during the one before: 33 % of
-// the wavefronts' time, 8192 x 4096 x 4096 in 175 to 185 us whatever the tile.  Now 129 to 132 us, 2.1 POP/s (a large bfloat16 product of the library
-// runs at 1.19 PFLOP/s).  Bound by the operands' way through LDS: for 32 of the
+// the wavefronts' time, 8192 x 4096 x 4096 in 175 to 185 us whatever the tile.  Now 129 to 140 us by the card, 2.0 to 2.1 POP/s (a large bfloat16 product of the
+// library runs at 1.19 PFLOP/s).  Bound by the operands' way through LDS: for 32 of the
 // reduction a workgroup reads 48 KB of it (384 clocks) and multiplies for 512, and the loads that fill it want the same port.
 // A row's 64 bytes are stored with their 16-byte chunk c at slot c ^ ((row >> 2) & 3), by choosing which chunk a lane asks for: sixteen
 // consecutive rows read with the same c touch all 64 banks once.  The weights come in the order of the instruction's lanes.
@@ -293,10 +293,13 @@ static int32_t launch_tile(LinearI8 a, hipStream_t stream) {
 // A workgroup of 16 wavefronts has a CU to itself and stays for many tiles.  Eight of them fetch the rows of the next tile and put them on
 // the grid, eight multiply this tile, and they meet at one barrier a tile.  With every wavefront doing both in turn and
 // two workgroups on a CU all read at once and then all multiplied at once: 602 + 602 bfloat16 columns to 256, 186 000 rows, took the
-// sum of the two (95 us to read, 53 to multiply, 41 to store).  Now 163 us, 3.3 TB/s: the fetching half takes 120 us by itself (two of its wavefronts
-// a SIMD, 70 us of it arithmetic), the multiplying half 88, and they share the vector unit.
-// LDS: two buffers of source, block of 32 rows, group of 16 k, row, 16 bytes; row r of group g at slot r ^ 4 (g mod 8), so that the groups of
-// four rows that a wavefront writes at once, 512 bytes apart, spread over all banks.
+// sum of the two (95 us to read, 53 to multiply, 41 to store).  Now 158 to 171 us, 3.2 to 3.4 TB/s: the fetching half takes 120 us by itself (two of its wavefronts
+// a SIMD, 70 us of it arithmetic), the multiplying half 88.  No unit is full (vector 45 %, matrix 15 %): wavefronts wait for 62 % of their time, for
+// rows and at the barrier, and which of the two was not told apart.
+// LDS: two buffers of source, block of 32 rows, group of 16 k, row, 16 bytes; row r of group g at slot r ^ 4 (g mod 8), which spreads the groups of
+// four rows that a wavefront writes at once, 512 bytes apart.  Conflicts are left: 1.96 clocks an LDS instruction, 6 % of a CU's clocks.
+// Tiles of 64 rows keep 2 to 9 of 128 registers in scratch (12 to 40 bytes a lane); bfloat16 rows of 641 to 1024 columns that do not start on
+// 16 bytes 30 to 136 (120 to 336 bytes).
 constexpr int kPanelBlocks = 16;     // blocks of 32 columns a workgroup may have
 
 template <int IN, int KC>
@@ -699,7 +702,8 @@ static int32_t launch_tiles(const LinearI8& a, hipStream_t stream) {
 // How a call runs, by its sizes alone.
 enum Route { kFew, kPanel, kTile };
 
-// us by route (MI355X):       rows x K -> N, sources      panel   tile 128
+// us by route (MI355X; the tiles before their last gain of 5 to 10 %):
+//                             rows x K -> N, sources      panel   tile 128
 //   bfloat16, up to 1024 columns  200 000 x 512 -> 512        140     187     (a launch before the tile kernel makes the codes)
 //                                 200 000 x 602 -> 256, two   172     315
 //                                 3000 x 1024 -> 4096          32      31
@@ -710,6 +714,8 @@ enum Route { kFew, kPanel, kTile };
 //                                 200 000 x 1024 -> 256       117     103
 //                                 1 000 000 x 128 -> 64       155     122
 //                                 50 000 x 602 -> 41           21      20
+// Not measured on both sides: float rows of up to 1024 columns with outputs wider than 512, other than the 3000 rows above, and 33 to 200 of them
+// (fewer than 8 tiles leave dies of the panel kernel's idle).
 //   32 rows x 4096 -> 4096: 7.8 with the kernel for few rows, 13 with tiles of 64; 8 rows from bfloat16 9.1 and 16.7.
 static Route route_of(int32_t n_active, int32_t K, int32_t N, bool codes) {
     if (n_active <= kFewRows) return kFew;

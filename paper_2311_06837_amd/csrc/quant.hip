@@ -1,8 +1,9 @@
 // Rows and weights on the 8-bit grid of gnn_linear_i8_fwd.
 //   a = max_k |x_k|,   scale = a / 127,   q_k = the whole number nearest to 127 x_k / a (ties to even)
 // The largest code is 127 on either side, so a sum of products of codes is symmetric and -128 never appears.
-// Which code is the nearest is decided exactly: a value that lands within 1e-4 of a border between two codes in 32 bits (one in 5000)
-// is divided again in 64 bits, where 127 x is exact and the quotient of two floats cannot round across a border.
+// Which code is the nearest is decided exactly: a float that lands within 2e-5 of a border between two codes in 32 bits (one in 25 000; eight
+// at a time) is divided again in 64 bits, where 127 x is exact and the quotient of two floats cannot round across a border.  bfloat16
+// never needs that (see codes_of).
 // A row below 2^-120 becomes zeros (127 / a would not be finite); a row that holds an infinity or NaN gets the scale NaN and
 // codes 0, so that it stays NaN in whatever is computed from it and no other row is touched.
 #include "quant.h"
@@ -11,8 +12,8 @@ namespace gnnhot {
 
 // ---- rows ----------------------------------------------------------------------------------------------------------
 // LR lanes own a row; lane sl holds the groups of eight sl, sl + LR, ... of it in registers (NV of them): one read of the row, one store
-// of its codes.  LR and NV are picked so that few lanes idle beyond the row's end (602 columns are 76 groups: 16 lanes x 5).  Bound: HBM.  With the values written too: 1M rows of 1024 bfloat16 860 to 1000 us by the card (5.1 to 6 TB/s), 186 000 listed rows of 602 floats, whose
-// rows start on 8 bytes only, 235 to 280 us (3.6 to 4.3 TB/s).
+// of its codes.  LR and NV are picked so that few lanes idle beyond the row's end (602 columns are 76 groups: 16 lanes x 5).  Bound: HBM.  With the values written too: 1M rows of 1024 bfloat16 890 to 900 us (860 to 1000 by the card; 5.1 to 6 TB/s),
+// 186 000 listed rows of 602 floats, whose rows start on 8 bytes only, 278 us (235 to 280; 3.6 to 4.3 TB/s).
 template <int DT, int LR, int NV, int AL>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantRows a) {
     constexpr int RPW = 64 / LR;
@@ -126,7 +127,7 @@ int32_t quantize_rows(const QuantRows& a, int32_t dtype, hipStream_t stream) {
 // ---- weights -------------------------------------------------------------------------------------------------------
 // Two launches, so that the reduction over K is spread over the chip: largest bit pattern of each column over kSplitK rows, then
 // the grid of each column from its few partial maxima, codes and layout (the second read comes from the caches).  4096 x 1031 floats with values
-// 8 + 13 us: bound by latency, a chain of two dependent loads a launch.
+// 8.3 + 13.3 us: bound by latency, a chain of two dependent loads a launch.
 constexpr int kSplitK = 64;
 
 template <int DT>

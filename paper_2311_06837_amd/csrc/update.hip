@@ -89,8 +89,8 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, ui
 // ---- norm of all gradients ---------------------------------------------------------------------------------------
 // Sum of squares in 64 bits: a square of a float is exact there, so the sum is good to about n 2^-53 whatever its order and
 // its 32-bit root does not depend on the split.  Bound: HBM, one read of the gradients (the 64-bit multiply-adds are a
-// twentieth of what the bytes take).  59M floats in 558 tensors 40 us (5.9 TB/s, part of it from the last-level cache), 247M 176 us;
-// 0.46M floats 5.6 us, the two launches.
+// twentieth of what the bytes take).  59M floats in 558 tensors 36 us in a loop of its own (6.5 TB/s, part of it from the last-level cache, which
+// holds 256 MB), 78 us after a step that moved 942 MB (3.0 TB/s); 247M 213 us after a step (4.6 TB/s); 0.46M 3.3 us.
 template <int DT, bool VEC>
 __device__ __forceinline__ double square_range(const void* g, int64_t i0, int64_t i1) {
     double s = 0.0;
@@ -150,7 +150,8 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const gnn_param* __restr
 }
 
 // A launch of its own: a count of finished workgroups in device memory (one launch) costs 28 ns for each of them, one after the other -
-// 58 us for the 1960 workgroups of a 59 MB model, where the sum itself takes 15.
+// 58 us for the 1960 workgroups of a model of 59 MB, where the sum itself takes 15.  A model of 452 chunks was faster with the count: the two
+// kernels took 6.5 us together and take 9 with this launch (2 us and the gap); a line between the two forms was not measured.
 __global__ __launch_bounds__(256) void norm_state_kernel(const double* __restrict__ part, int32_t n_part, float grad_scale, float max_norm,
                                                          gnn_step_state* __restrict__ state) {
     __shared__ double lds[4];
@@ -233,8 +234,8 @@ __device__ __forceinline__ float v_code(float x) {
 // The draw is a function of (seed, step, tensor, element) alone: products of 32 bits by odd constants (the fractions of the golden ratio and of
 // the roots of 3 and 2), their halves folded onto each other; m takes the upper 23 bits of the element's number, v the lower 23 in
 // reverse.  Uniform and without correlation between elements, steps, tensors and the two (1M draws in 4096 cells each).
-// What it costs: four products a draw at a quarter of the vector unit's rate, which the step is close to being bound by: 247M elements 889 to 896 us
-// (819 with nearest codes), 59M 239 to 260 (183).
+// What it costs: four products a draw at a quarter of the vector unit's rate, which the step is close to being bound by: 247M elements 889 to 914 us
+// (819 with nearest codes), 59M 239 to 260 (183 to 207).
 constexpr uint32_t kDraw[3] = {0x9E3779B9u, 0xBB67AE85u, 0x6A09E667u};
 __device__ __forceinline__ uint32_t fold(uint32_t x, uint32_t c) {
     const uint64_t p = (uint64_t)x * c;
@@ -305,7 +306,7 @@ __device__ __forceinline__ void roots(const float (&v)[4], float (&r)[4]) {
 
 // A wavefront takes 256 elements at a time, four a lane: 16-byte loads and stores of floats, and exactly one block of an 8-bit state, whose
 // largest value is then a reduction inside the wavefront.  Bound: HBM.  28 bytes an element with float states, 16 with 8-bit states:
-// 247M elements in 8 bits 840 us (4.7 TB/s; a copy of 4 GB runs at 4.8), 59M 190 to 218 us, 0.46M with float states 5.5 us.
+// 247M elements in 8 bits, nearest codes, 819 us (4.8 TB/s, the rate of a copy of 4 GB; the vector unit is busy for 84 %), 59M 183 to 207 us, 0.46M with float states 5.4 us.
 // With the codes found by IEEE roots and branches the 8-bit form was bound by the vector unit instead: 938 and 261 us.
 struct AdamTensor {
     void* param;

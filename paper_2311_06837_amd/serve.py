@@ -2,6 +2,9 @@
 
 The order of calls is the forward pass of the model (paper section 2.1's layer equation under section 6's masks), with
 gnn_linear_i8_fwd in the place of gnn_linear_fwd: aggregation in the model's type, the feature transform in integers.
+Every layer aggregates first.  A model that transforms its narrowing layers first gathers narrower rows, which is worth more than the
+integers: ms of model.forward / Int8Answers.forward 13.8 / 20.4 (GraphSAGE 602-256-256-41, float32, 114M edges),
+31.2 / 30.5 (GCN 100-256-256-47, float32, 125M), 5.7 / 6.7 (GraphSAGE of eight layers of 128, bfloat16, 20M).
 """
 from __future__ import annotations
 
@@ -15,7 +18,7 @@ class Int8Answers:
     """Logits of a MaskedGNN's targets from 8-bit weights.
 
     model   its graph, active sets (build_active_sets or step has run), input and parameters are used; its activations are not
-            touched.  Layers run in the paper's order (aggregate, then transform).
+            touched.  Layers run in the paper's order (aggregate, then transform), whatever the model's.
     refresh puts the model's present weights on the grid; call it again after an update of the weights.
     """
 
