@@ -176,6 +176,30 @@ def test_nearest_states_freeze():
     assert np.median(v8[:64] / v[:64]) > 30 and np.median(v8[64:128] / v[64:128]) > 30 and m8[64:128].any()
 
 
+def test_twelve_thousand_steps_of_stationary_and_of_rising_gradients():
+    """A block of normal gradients of sizes e^-4 .. 1: codes from about 30 on, spread 0.26 and less, of a median of 256 1.25 / 16 of that and of
+    the smallest 64 1.25 / 8.  And one of constant gradients, 64 of which rise from 0.2 to 0.6 beside a 1: code 197, spread 0.1, of a mean of 64
+    an eighth; with nearest codes they stay at their old second moments, a ninth of the new."""
+    rng = np.random.default_rng(11)
+    size = np.exp(rng.uniform(-4, 0, 256))
+    still, rising, frozen = Definition(256), Definition(256, 1), Definition(256, 1, seed=0)
+    v, w = np.zeros(256), np.zeros(256)
+    for t in range(1, 12_001):
+        g = (rng.standard_normal(256) * size).astype(f32)
+        v = B2 * v + (1 - B2) * g.astype(np.float64) ** 2
+        still.step(g, t)
+        r = np.full(256, 0.3, f32)
+        r[:64], r[255] = 0.2 if t <= 1000 else 0.6, 1
+        w = B2 * w + (1 - B2) * r.astype(np.float64) ** 2
+        rising.step(r, t)
+        frozen.step(r, t)
+        if t in (1000, 4000, 12_000):
+            q = still.decoded()[1] / v
+            assert 0.9 <= np.median(q) <= 1.1 and 0.75 <= np.median(q[np.argsort(size)[:64]]) <= 1.33, (t, np.median(q))
+    assert 0.9 <= (rising.decoded()[1] / w)[:64].mean() <= 1.1
+    assert (frozen.decoded()[1] / w)[:64].mean() < 0.3
+
+
 def test_seeds_have_32_bits():
     for seed in (-1, 1 << 32):
         with pytest.raises(ValueError, match="rounding_seed"):
